@@ -185,7 +185,8 @@ struct TileSide {
     __device__ __forceinline__ void issue(int j, uint32_t lds, int wv) const
     {
         const uint32_t to = lds + (j * WAVES + wv) * 1024;
-        asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(v[j & 1] + j * jstep), "s"(rsrc) : "memory");
+        // (the compiler writes M0; a load with the LDS bit comes one wait state behind that at the earliest)
+        asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(v[j & 1] + j * jstep), "s"(rsrc) : "memory");
     }
 
     // ---- LDS to registers
