@@ -154,7 +154,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort(const void* __restric
     }
     // Pieces whose first place lies here.
     const int32_t from = bounds[0], to = bounds[kSortRows];
-    for (int32_t k = cdiv(from, kPiece) + (int32_t)threadIdx.x; k * kPiece < to; k += kSortThreads) {
+    for (int64_t k = cdiv(from, kPiece) + threadIdx.x; k * kPiece < to; k += kSortThreads) {  // (k * kPiece passes 32 bits behind the last)
         int lo = 0, hi = kSortRows;  // bounds[lo] <= place < bounds[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
@@ -180,10 +180,10 @@ __device__ __forceinline__ void add_rows(const T* __restrict__ dY, int64_t D, in
 {
     typedef T VT __attribute__((ext_vector_type(VN)));
     constexpr int U = 4;  // (8: 139 us for 132 at 16384 tokens, 32000 x 4096 bf16: fewer waves)
-    for (int32_t j = b; j < e; j += U) {
+    for (uint32_t j = b; j < (uint32_t)e; j += U) {  // (e is up to 2^31 - 1: j + u passes that)
         VT x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = j + u < e ? *(const VT*)(dY + (int64_t)sorted[j + u] * D + col) : (VT)(T)0.0f;
+        for (int u = 0; u < U; ++u) x[u] = j + u < (uint32_t)e ? *(const VT*)(dY + (int64_t)sorted[j + u] * D + col) : (VT)(T)0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
