@@ -770,13 +770,22 @@ __global__ __launch_bounds__(kLayThreads) void xent_gather(const T* __restrict__
     }
 }
 
-// dz as it is held, before it is rounded, from the sum of a logit.
+// dz as it is held, before it is rounded, from the sum of a logit.  (16-bit types: the lift goes into the exponent only where exp z alone
+// would run out of digits; beside it, an exponent near 0 would keep 19 binary places of its own, and 1 - p of a token whose target is
+// all but certain with it.)
 template <typename T>
 __device__ __forceinline__ float dz_of(float sum, float scale, const Row& row, bool target)
 {
+    constexpr float kUp = (float)(1 << kLift<T>);
     const float z = sum * scale - row.lse;
-    const float p = sizeof(T) == 4 ? lifted_exp<kLift<T>>(z) : __builtin_amdgcn_exp2f(z * kLog2e + (float)kLift<T>);
-    return row.g * (p - (target ? (float)(1 << kLift<T>) : 0.0f));
+    float p;
+    if constexpr (sizeof(T) == 4) {
+        p = lifted_exp<kLift<T>>(z);
+    } else {
+        const bool low = z < -60.0f;
+        p = __builtin_amdgcn_exp2f(z * kLog2e + (low ? (float)kLift<T> : 0.0f)) * (low ? 1.0f : kUp);
+    }
+    return row.g * (p - (target ? kUp : 0.0f));
 }
 
 // dz from shares of the logits.

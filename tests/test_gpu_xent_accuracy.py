@@ -1,0 +1,30 @@
+"""Cross entropy where digits are easily lost: tokens whose target is all but certain, weights of very different size, entries at the
+ends of the range.  Inputs are chosen so that logits are exact in f32; bounds follow from the roundings that remain.  E, U as in test_gpu_lm."""
+import pytest
+import torch
+
+from test_gpu_lm import DEV, E, TYPES, U, near, scd  # noqa: F401  (scd: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def confident(N, V, dtype):
+    """Token n has logit 0 for its target n and -c_n for the others, c_n = 12 .. 20 in eighths: 1 - p is V exp(-c_n)."""
+    c = 12.0 + (torch.arange(N, device=DEV) % 64) / 8.0
+    x = torch.diag(c).to(dtype)
+    w = torch.full((V, N), -1.0, device=DEV)
+    w[:N].fill_diagonal_(0.0)
+    return c.double(), x, w.to(dtype), torch.arange(N, device=DEV)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V", [(64, 64), (64, 2500), (200, 700)])
+def test_weight_gradient_of_confident_tokens(scd, dtype, N, V):  # noqa: F811
+    c, x, w, t = confident(N, V, dtype)
+    g = torch.full((N,), 0.375, device=DEV)
+    _, lse = scd.scd_xent(x, w, t)
+    _, dW = scd.scd_xent_grad(x, w, t, lse, g, want_dX=False)
+    # entry (n, n) of dW is one term, g (p_n - 1) c_n with p_n = exp(-lse_n); p is off by two steps of f32 below 1, dz has at
+    # least the type's digits, and so has the result
+    want = 0.375 * torch.expm1(-lse.double()) * c
+    near(dW[:N].diagonal(), want, 0.375 * c * 2 * E + 2.02 * U[dtype] * want.abs() + 4 * E * want.abs())
