@@ -198,9 +198,10 @@ __global__ __launch_bounds__(kTThreads) void xent_forward32(Operand<T> W, Operan
 __device__ __forceinline__ void write_loss(int64_t n, float top, double sum, float zt, int64_t target, int64_t V, int64_t ignore, float* __restrict__ loss,
                                            float* __restrict__ lse)
 {
-    const float l = (float)((double)top + log(sum));
-    lse[n] = l;
-    loss[n] = target == ignore ? 0.0f : (uint64_t)target < (uint64_t)V ? l - zt : __builtin_nanf("");
+    const double l = log(sum);
+    lse[n] = (float)((double)top + l);
+    // (not lse - zt: lse rounded to f32 has a step of 2^-19 from 16 on, and the loss of a likely target is far below that)
+    loss[n] = target == ignore ? 0.0f : (uint64_t)target < (uint64_t)V ? (float)((double)top - (double)zt + l) : __builtin_nanf("");
 }
 
 // TOKENS tokens a workgroup, the threads of a token each take every so many strips: first the largest logit, then the sum in

@@ -28,3 +28,20 @@ def test_weight_gradient_of_confident_tokens(scd, dtype, N, V):  # noqa: F811
     # least the type's digits, and so has the result
     want = 0.375 * torch.expm1(-lse.double()) * c
     near(dW[:N].diagonal(), want, 0.375 * c * 2 * E + 2.02 * U[dtype] * want.abs() + 4 * E * want.abs())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V,shift", [(64, 64, 0), (64, 2500, 200), (300, 700, 200), (3, 40000, 200)])
+def test_losses_of_confident_tokens(scd, dtype, N, V, shift):  # noqa: F811
+    """The target's logit is the largest: the loss is log(1 + the others' exponentials), whatever the logit itself is."""
+    c, x, w, t = confident(N, V, dtype)
+    x = torch.cat([x, torch.ones((N, 1), dtype=dtype, device=DEV)], 1)
+    w = torch.cat([w, torch.full((V, 1), float(shift), device=DEV).to(dtype)], 1)  # adds `shift` to every logit, exactly
+    loss, lse = scd.scd_xent(x, w, t)
+    others = (V - 1) * torch.exp(-c)
+    want = torch.log1p(others)
+    # a lane adds at most 32 exponentials in f32, two more sums and a product follow, the rest is in 64 bits: 35 roundings of a sum
+    # that holds the target's 1; the others' exponents are up to 20 log2 e = 29, off by half a step each
+    tol = 36 * E + 60 * E * others
+    near(loss, want, tol + E * want)
+    near(lse, want + shift, tol + E * (want + shift))
