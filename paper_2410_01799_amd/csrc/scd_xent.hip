@@ -248,13 +248,19 @@ constexpr int kListThreads = 1024;
 
 __device__ __forceinline__ bool counts_for(int64_t t, int64_t V, int64_t ignore, float g) { return t != ignore && (uint64_t)t < (uint64_t)V && g != 0.0f; }
 
+// The bits of |g| for the largest of them; a g that is not finite shows in its own token's terms and says nothing of the others.
+__device__ __forceinline__ uint32_t weight_of(float g)
+{
+    const uint32_t m = __float_as_uint(g) & 0x7FFFFFFFu;
+    return m < 0x7F800000u ? m : 0u;
+}
+
 // From the number of tokens that count and the bits of their largest |g|.
 __device__ __forceinline__ Active active_of(int32_t count, uint32_t top, int lift)
 {
     Active a;
     a.count = count;
-    // (no g at all, or one that is not finite: as they are)
-    a.ref = top == 0 || top >= 0x7F800000u ? 1.0f : fmaxf(__uint_as_float(top), 0x1p-100f);
+    a.ref = top == 0 ? 1.0f : fmaxf(__uint_as_float(top), 0x1p-100f);  // (no finite g at all: as they are)
     a.inv = ldexpf(a.ref, -lift);
     return a;
 }
@@ -275,7 +281,7 @@ __global__ __launch_bounds__(kListThreads) void xent_list(const void* __restrict
             const int64_t t = index_at(targets, index_bytes, i);
             const float gi = g[i];
             in = counts_for(t, V, ignore, gi);
-            const uint32_t m = in ? __float_as_uint(gi) & 0x7FFFFFFFu : 0u;
+            const uint32_t m = in ? weight_of(gi) : 0u;
             top = m > top ? m : top;
         }
         const uint64_t mask = __ballot(in);
@@ -712,7 +718,7 @@ __global__ __launch_bounds__(kLayThreads) void xent_gather(const T* __restrict__
         for (int64_t i = threadIdx.x; i < a.N; i += kLayThreads) {
             const float g = a.g[i];
             const bool c = counts_for(index_at(a.targets, a.index_bytes, i), a.V, a.ignore, g);
-            const uint32_t m = c ? __float_as_uint(g) & 0x7FFFFFFFu : 0u;
+            const uint32_t m = c ? weight_of(g) : 0u;
             top = m > top ? m : top;
             na += c;
             nb += c && i < r0;

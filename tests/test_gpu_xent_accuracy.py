@@ -3,7 +3,7 @@ ends of the range.  Inputs are chosen so that logits are exact in f32; bounds fo
 import pytest
 import torch
 
-from test_gpu_lm import DEV, E, TYPES, U, near, scd  # noqa: F401  (scd: the fixture)
+from test_gpu_lm import DEV, E, TYPES, U, near, same, scd  # noqa: F401  (scd: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,22 @@ def test_losses_of_confident_tokens(scd, dtype, N, V, shift):  # noqa: F811
     tol = 36 * E + 60 * E * others
     near(loss, want, tol + E * want)
     near(lse, want + shift, tol + E * (want + shift))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N", [20, 70])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_weight_that_is_not_finite_stays_with_its_token(scd, dtype, N, bad):  # noqa: F811
+    V, D = 72, 64
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    x, w = (torch.randn((n, D), generator=gen, device=DEV).to(dtype) for n in (N, V))
+    t = torch.arange(N, device=DEV) % V
+    g = 100.0 + 200.0 * torch.rand(N, generator=gen, device=DEV)
+    _, lse = scd.scd_xent(x, w, t)
+    g[3] = 0.0
+    want, _ = scd.scd_xent_grad(x, w, t, lse, g, want_dW=False)
+    g[3] = bad
+    got, _ = scd.scd_xent_grad(x, w, t, lse, g, want_dW=False)
+    rest = torch.arange(N, device=DEV) != 3
+    assert not torch.isfinite(got[3]).any() and torch.isfinite(want).all()
+    same(got[rest], want[rest])  # (held relative to the largest finite weight)
