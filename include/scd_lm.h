@@ -77,7 +77,8 @@ int scd_xent(const void* X, const void* W, scd_real dt, int64_t N, int64_t D, in
  * dW = scale dz^T X (V x D), both of dt, written whole; either may be NULL (not both).  lse is scd_xent's.  The logits are
  * formed again, in pieces of the vocabulary.  A row with g_i = 0, t_i == ignore or t_i outside 0 .. V-1 counts for nothing,
  * whatever it holds: its dX is zero.  dz is rounded to dt before the products with W and X (16-bit types: the matrix cores
- * take 16-bit operands); f16 holds it relative to the largest |g_i|, so that g carries no range of its own. */
+ * take 16-bit operands), held relative to the largest finite |g_i|, so that g carries no range of its own: in f16 in steps of 2^-39 of
+ * that where its digits would be finer. */
 size_t scd_xent_grad_workspace_bytes(scd_real dt, int64_t N, int64_t D, int64_t V);
 int scd_xent_grad(const void* X, const void* W, scd_real dt, int64_t N, int64_t D, int64_t V, const void* targets, int index_bytes,
                   int64_t ignore, float scale, const float* lse, const float* g, void* dX, void* dW, void* workspace,

@@ -30,7 +30,7 @@ struct Active {
 template <typename T>
 constexpr int kLift = 24;
 template <>
-constexpr int kLift<_Float16> = 10;  // f16 ends at 65504
+constexpr int kLift<_Float16> = 15;  // f16 ends at 65504; |dz| is at most 2^15
 
 // 2^LIFT exp(x) for x <= 0 and a little above.
 template <int LIFT>

@@ -47,6 +47,24 @@ def test_losses_of_confident_tokens(scd, dtype, N, V, shift):  # noqa: F811
     near(lse, want + shift, tol + E * (want + shift))
 
 
+@pytest.mark.parametrize("N", [20, 70, 300])
+def test_f16_gradients_of_tokens_of_little_weight(scd, N):  # noqa: F811
+    """Rows of W are unit vectors, so that dX is dz itself; all tokens but one weigh 2^-27 of that one."""
+    V = 72
+    x = torch.randn((N, V), generator=torch.Generator(device=DEV).manual_seed(5), device=DEV).half()
+    w, t = torch.eye(V, device=DEV).half(), torch.arange(N, device=DEV) % V
+    ref = 2.0 ** 15
+    g = ref * 2.0 ** -27 * (1.0 + torch.rand(N, generator=torch.Generator(device=DEV).manual_seed(6), device=DEV))
+    g[0] = ref
+    _, lse = scd.scd_xent(x, w, t)
+    dX, _ = scd.scd_xent_grad(x, w, t, lse, g, want_dW=False)
+    p = (x.double() - lse.double()[:, None]).exp()
+    want = g.double()[:, None] * (p - torch.nn.functional.one_hot(t, V).double())
+    # p: exponents below 16, two steps of it; dz: the type's digits, or steps of 2^-24 of numbers up to 2^15; the result: its digits or steps
+    tol = g.double()[:, None] * 24 * E + 2.02 * U[torch.float16] * want.abs() + 2.0 ** -39 * ref + 2.0 ** -25
+    near(dX, want, tol)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("N", [20, 70])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
