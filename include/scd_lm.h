@@ -67,7 +67,7 @@ int scd_q8_linear(const void* X, scd_real dt, int64_t M, int64_t K, const int8_t
  *     lse_i = log sum_v exp z_iv (every row),   loss_i = lse_i - z_{i,t_i}      (f32, N each)
  * loss is 0 where t_i == ignore, NaN where t_i is another value outside 0 .. V-1.  A logit that is NaN or +infinity makes its
  * row's lse and loss NaN.  In f32, D and V from 64 on, products are of three parts of bf16: entries below 2^-102 may lose some
- * of their 24 bits, finite ones beyond 3.39e38 may be taken for that or, in gradients, for infinite.  Logits are formed tile by
+ * of their 24 bits, finite ones beyond 3.39e38 may be taken for that.  Logits are formed tile by
  * tile and not kept: the work space holds a few sums for each row and tile (and, where there are few logits in all, these). */
 size_t scd_xent_workspace_bytes(scd_real dt, int64_t N, int64_t D, int64_t V);
 int scd_xent(const void* X, const void* W, scd_real dt, int64_t N, int64_t D, int64_t V, const void* targets, int index_bytes,
@@ -78,7 +78,9 @@ int scd_xent(const void* X, const void* W, scd_real dt, int64_t N, int64_t D, in
  * formed again, in pieces of the vocabulary.  A row with g_i = 0, t_i == ignore or t_i outside 0 .. V-1 counts for nothing,
  * whatever it holds: its dX is zero.  dz is rounded to dt before the products with W and X (16-bit types: the matrix cores
  * take 16-bit operands), held relative to the largest finite |g_i|, so that g carries no range of its own: in f16 in steps of 2^-39 of
- * that where its digits would be finer. */
+ * that where its digits would be finer.  In bf16 and f32 it is lifted by 2^24 beside that, against the smallest numbers of the
+ * type, and undone after the sums, which are therefore infinite where sum |dz x| / max |g| reaches 2^104 (2e31): entries of X and W
+ * below 2^100 keep clear of it. */
 size_t scd_xent_grad_workspace_bytes(scd_real dt, int64_t N, int64_t D, int64_t V);
 int scd_xent_grad(const void* X, const void* W, scd_real dt, int64_t N, int64_t D, int64_t V, const void* targets, int index_bytes,
                   int64_t ignore, float scale, const float* lse, const float* g, void* dX, void* dW, void* workspace,

@@ -3,7 +3,7 @@ ends of the range.  Inputs are chosen so that logits are exact in f32; bounds fo
 import pytest
 import torch
 
-from test_gpu_lm import DEV, E, TYPES, U, near, same, scd  # noqa: F401  (scd: the fixture)
+from test_gpu_lm import DEV, E, TYPES, U, check_xent, near, same, scd, xent_inputs  # noqa: F401  (scd: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +82,15 @@ def test_a_weight_that_is_not_finite_stays_with_its_token(scd, dtype, N, bad):  
     rest = torch.arange(N, device=DEV) != 3
     assert not torch.isfinite(got[3]).any() and torch.isfinite(want).all()
     same(got[rest], want[rest])  # (held relative to the largest finite weight)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,D,V", [(7, 72, 300), (300, 72, 300), (40, 256, 2500), (600, 1030, 700)])
+def test_gradients_with_very_large_entries(scd, dtype, N, D, V):  # noqa: F811
+    """Entries just below the 2^100 that the header names, in one column of X, and in another of W, where the other matrix is zero."""
+    x, w, t, g = xent_inputs(N, D, V, dtype, 300, ignored=0.1)
+    x[:, 1] = x[:, 1].clamp(-1, 1) * 2.0 ** 99
+    w[:, 1] = 0
+    w[:, 2] = w[:, 2].clamp(-1, 1) * 2.0 ** 99
+    x[:, 2] = 0
+    check_xent(scd, x, w, t, g)
