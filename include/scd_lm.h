@@ -13,7 +13,9 @@
  *    starts are aligned to 16 bytes are faster.  All sums are formed in f32 or wider (integer products: exactly, in
  *    int32) and rounded to the type once.
  *  - Index arrays (tokens, targets) hold int32 (index_bytes 4) or int64 (8).
- *  - Every result is the same bits from run to run: no float atomics, every sum in an order set by the sizes alone.
+ *  - Every result is the same bits from run to run: no float atomics, every sum in an order set by the sizes (cross entropy with rows
+ *    of whole 16 bytes: and by whether W, in scd_xent also X, begins at a multiple of 16; if not, plainer sums serve the call, in
+ *    f32 throughout).
  *  - Row counts may be 0 (nothing to do; gradients of weights are then zero).
  *  - SCD_EINVAL: null pointers, sizes below 1 (row counts: below 0) or above 2^31 - 1, an unknown type, a work space that
  *    is too small or misaligned.  SCD_EHIP: a launch failed.  Nothing is enqueued on SCD_EINVAL.

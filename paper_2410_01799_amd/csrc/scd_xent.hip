@@ -11,8 +11,8 @@
 //
 // Two forms.  The tile of scd_lm_tile.h takes 16-bit types, dz held in the type, and f32, dz in f32, on the bf16 instruction (sums of a
 // few terms on the f32 instruction).  Rows that are no multiple of 16 bytes are copied to the work space first, W a piece at a time.
-// tile32 below, the f32 matrix instruction from operands of any type, alignment and order with dz in f32, takes arrays that begin at
-// odd addresses.
+// tile32 below, the f32 matrix instruction from operands of any type, alignment and order with dz in f32, takes weights (in the forward:
+// and hidden states) that begin at odd addresses.
 #include "scd_lm_tile.h"
 
 namespace scd {
@@ -1331,7 +1331,7 @@ Shape shape_of(int dt, int64_t N, int64_t D, int64_t V)
     return s;
 }
 
-// Whether the tile takes a call.
+// Whether the tile takes operands at these addresses (one that is copied in any case: nullptr).
 bool tile_takes(const Shape& s, const void* X, const void* W)
 {
     if (s.ld * s.bytes > kTileMaxPitch) return false;
@@ -1642,7 +1642,7 @@ hipError_t grad_t(const GradArgs& a, const Shape& s, hipStream_t st)
     const GradSpace sp = grad_space(s);
     int32_t* list = (int32_t*)(a.ws + sp.list);
     Active* active = (Active*)(a.ws + sp.active);
-    if (tile_takes(s, a.X, a.W)) {
+    if (tile_takes(s, nullptr, a.W)) {  // (X's rows are gathered)
         if constexpr (sizeof(T) == 2)
             if (s.dz_planes == 2) return grad_tile_t<T, H, Twice<H>>(a, s, sp, st);
         return grad_tile_t<T, H, H>(a, s, sp, st);

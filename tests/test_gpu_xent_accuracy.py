@@ -3,7 +3,7 @@ ends of the range.  Inputs are chosen so that logits are exact in f32; bounds fo
 import pytest
 import torch
 
-from test_gpu_lm import DEV, E, TYPES, U, check_xent, near, same, scd, xent_inputs  # noqa: F401  (scd: the fixture)
+from test_gpu_lm import DEV, E, TYPES, U, check_xent, near, off_by_one, same, scd, xent_inputs  # noqa: F401  (scd: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +94,12 @@ def test_gradients_with_very_large_entries(scd, dtype, N, D, V):  # noqa: F811
     w[:, 2] = w[:, 2].clamp(-1, 1) * 2.0 ** 99
     x[:, 2] = 0
     check_xent(scd, x, w, t, g)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,D,V", [(5, 264, 530), (150, 264, 530), (300, 520, 4097)])
+def test_gradients_do_not_depend_on_where_the_hidden_states_lie(scd, dtype, N, D, V):  # noqa: F811
+    x, w, t, g = xent_inputs(N, D, V, dtype, 310)
+    _, lse = scd.scd_xent(x, w, t)
+    for a, b in zip(scd.scd_xent_grad(off_by_one(x), w, t, lse, g), scd.scd_xent_grad(x, w, t, lse, g)):
+        same(a, b)
