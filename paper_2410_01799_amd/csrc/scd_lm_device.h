@@ -3,7 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "scd_lm.h"
+#include "scd_lm_shape.h"
 
 namespace scd {
 
@@ -23,8 +23,6 @@ inline bool index_ok(int bytes) { return bytes == 4 || bytes == 8; }
 inline bool dim_ok(int64_t d) { return d >= 1 && d <= kMaxDim; }
 inline bool rows_ok(int64_t d) { return d >= 0 && d <= kMaxDim; }
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-inline size_t up(size_t x, size_t unit) { return (x + unit - 1) / unit * unit; }
-__host__ __device__ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // A launch has fewer than 2^32 threads along x.
 inline bool grid_ok(int64_t groups, int64_t threads) { return groups >= 1 && groups <= (int64_t)0xFFFFFFFF / threads; }
 

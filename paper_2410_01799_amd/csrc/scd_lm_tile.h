@@ -42,8 +42,6 @@ struct TileRows {
     int64_t pitch, rows, bytes, plane = 0;
 };
 
-constexpr int64_t kTileMaxPitch = (int64_t)1 << 22;  // 256 rows of it keep a 32-bit offset
-
 struct OpBf16 {
     typedef __bf16 In __attribute__((ext_vector_type(8)));
     typedef v4f Acc;
@@ -102,8 +100,6 @@ struct OpSplit {
         for (int p = 0; p < 3; ++p) part[p] = __builtin_bit_cast(In, out[p]);
     }
 };
-
-constexpr int kTileStep = 128;  // bytes along k of a step
 
 // One operand's side of the tile, of PLANES planes of values of ES bytes: F fragments of 16 a wave, W waves across, T = 16 F W rows;
 // WAVES waves in all.  ALONG: rows of memory run along k.  BLOCKED: the rows of a wave are dealt to its fragments four at a time, a block of 4 F for each
@@ -445,20 +441,6 @@ __device__ __forceinline__ void tile_order(int64_t index, int64_t na, int64_t nb
     const int64_t width = nb - first < group ? nb - first : group, r = t - strip * group * na;
     *ta = r / width;
     *tb = first + r % width;
-}
-
-// Which of the square tiles of 256, 128 and 64 a product of na x nb entries takes: the one that the compute
-// units are done with first, each with its share of the tiles one after the other.  A smaller tile takes more time for its
-// entries (less is multiplied between two reads), relative to that of 256: rate128, rate64; largest: 128 leaves out that of 256.
-inline int pick_tile(int64_t na, int64_t nb, double rate128, double rate64, int largest = 256)
-{
-    int best = 0;
-    double least = 0;
-    for (int t = largest; t >= 64; t /= 2) {
-        const double turns = (double)cdiv(cdiv(na, t) * cdiv(nb, t), 256), cost = turns * t * t / (t == 256 ? 1.0 : t == 128 ? rate128 : rate64);
-        if (best == 0 || cost < least) best = t, least = cost;
-    }
-    return best;
 }
 
 // Where tile ta of na begins its steps if it has its rows of A to itself (one tile holds all of b): spread evenly.

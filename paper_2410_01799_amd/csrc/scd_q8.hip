@@ -216,34 +216,10 @@ hipError_t tile_t(const int8_t* xq, const float* xs, int64_t M, int64_t K, const
 // own stretch of the weights on the way to its registers at once, the next channels' already while the waves' sums meet in LDS.
 // OWN > 0: the tokens, at most OWN, are not yet in 8 bits; every workgroup does that for itself while its first weights are on
 // the way, which takes less than a launch.  They lie in LDS then, and are read from there.
-constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave, kFewTokens = 16, kFewChannels = 16;
+constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave, kFewTokens = kQ8FewTokens, kFewChannels = 16;
 constexpr int kFewFlight = 8;  // steps of 64 bytes that a wave has in flight
-constexpr int kFewPad = 64;    // bytes between the tokens' rows in LDS
-constexpr int kFewLds = 48 * 1024;    // for the rows of up to four tokens, which all threads round together
-constexpr int kFewLongest = 16384;    // bytes of a row there, at most
-constexpr int kManyLds = 112 * 1024;  // for the rows of more, which the waves round one by one
-
-// How the workgroups put the tokens into 8 bits themselves: 1, 2 or 4: all threads, so many tokens at once; kFewTokens: a token a
-// wave; 0: not at all.
-inline int few_owns(int64_t M, int64_t K)
-{
-    const int64_t row = scd_q8_stride(K) + kFewPad;
-    const int together = M <= 1 ? 1 : M == 2 ? 2 : 4;
-    if (M <= 4 && row <= kFewLongest + kFewPad && together * row <= kFewLds) return together;
-    return M <= kFewTokens && M * row <= kManyLds ? kFewTokens : 0;
-}
-
-// Whether q8_few_kernel takes so many tokens at all.  It reads a few MiB at once with the least latency; large weights stream
-// faster through the tile once there is more than a token or two to multiply them with (measured: 14336 x 14336, 4 tokens, 54 us
-// here and 40 there; 14336 x 4096, 16 tokens, 25 and 22, 8 tokens 21 and 22; 4096 x 14336, 16 tokens, 27 and 32).
-inline bool few_takes(int64_t M, int64_t K, int64_t N)
-{
-    const int64_t bytes = N * scd_q8_stride(K);
-    return M <= kFewTokens && !(M > 2 && bytes >= (96 << 20)) && !(M > 8 && N >= 8192 && bytes >= (48 << 20));
-}
-
 // LDS of the tokens' rows.
-inline size_t few_lds(int own, int64_t M, int64_t K) { return (size_t)(own == kFewTokens ? M : own) * (size_t)(scd_q8_stride(K) + kFewPad); }
+inline size_t few_lds(int own, int64_t M, int64_t K) { return (size_t)(own == kFewTokens ? M : own) * (size_t)(scd_q8_stride(K) + kQ8FewPad); }
 constexpr int kFewGroups = 512;  // workgroups, at most: two on each compute unit
 
 template <typename T>
@@ -275,7 +251,7 @@ __global__ __launch_bounds__(kFewThreads) void q8_few_kernel(FewTokens<T> X, int
     int64_t n0 = (int64_t)blockIdx.x * kFewChannels;
     weights(n0, s0);
     float sx = 0.0f;
-    const int pitch = (int)stride + kFewPad;
+    const int pitch = (int)stride + kQ8FewPad;
     if constexpr (OWN == kFewTokens) {
         constexpr int VN = 16 / sizeof(T);
         typedef typename Vec<T>::V VT;
@@ -335,7 +311,7 @@ __global__ __launch_bounds__(kFewThreads) void q8_few_kernel(FewTokens<T> X, int
         constexpr int VN = 16 / sizeof(T);
         typedef typename Vec<T>::V VT;
         typedef int8_t VQ __attribute__((ext_vector_type(VN)));
-        constexpr int kLongest = kFewLds / OWN < kFewLongest ? kFewLds / OWN : kFewLongest;
+        constexpr int kLongest = kQ8FewLds / OWN < kQ8FewLongest ? kQ8FewLds / OWN : kQ8FewLongest;
         constexpr int kFewHeld = (kLongest / VN + kFewThreads - 1) / kFewThreads;  // chunks of a token that a thread holds
         VT held[OWN][kFewHeld];
         uint32_t top[OWN];
@@ -440,7 +416,7 @@ hipError_t few_t(const FewTokens<T>& X, int64_t M, int64_t K, const int8_t* wq, 
     const size_t lds = OWN ? few_lds(OWN, M, K) : 0;
     const int64_t groups = cdiv(N, kFewChannels), most = lds > 56 * 1024 ? kFewGroups / 2 : kFewGroups, grid = groups < most ? groups : most;
     if (OWN == kFewTokens) {
-        const hipError_t e = hipFuncSetAttribute((const void*)q8_few_kernel<T, OWN>, hipFuncAttributeMaxDynamicSharedMemorySize, kManyLds);
+        const hipError_t e = hipFuncSetAttribute((const void*)q8_few_kernel<T, OWN>, hipFuncAttributeMaxDynamicSharedMemorySize, kQ8ManyLds);
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL((q8_few_kernel<T, OWN>), dim3((unsigned)grid), dim3(kFewThreads), (unsigned)lds, st, X, (int)M, K, scd_q8_stride(K), wq, ws, N,
@@ -457,11 +433,13 @@ template <typename T>
 hipError_t matmul_t(const int8_t* xq, const float* xs, int64_t M, int64_t K, const int8_t* wq, const float* ws, int64_t N, const void* bias, void* y,
                     hipStream_t st)
 {
-    if (few_takes(M, K, N)) return few_t<T, 0>(FewTokens<T>{xq, xs, nullptr, false}, M, K, wq, ws, N, bias, y, st);
-    if (M <= 64) return tile_t<T, Narrow>(xq, xs, M, K, wq, ws, N, bias, y, st);
-    const int t = pick_tile(N, M, 0.8, 0.45);
-    if (t == 256) return tile_t<T, Large>(xq, xs, M, K, wq, ws, N, bias, y, st);
-    return t == 128 ? tile_t<T, Middle>(xq, xs, M, K, wq, ws, N, bias, y, st) : tile_t<T, Small>(xq, xs, M, K, wq, ws, N, bias, y, st);
+    switch (q8_form(M, K, N)) {
+        case Q8Form::few: return few_t<T, 0>(FewTokens<T>{xq, xs, nullptr, false}, M, K, wq, ws, N, bias, y, st);
+        case Q8Form::narrow: return tile_t<T, Narrow>(xq, xs, M, K, wq, ws, N, bias, y, st);
+        case Q8Form::t256: return tile_t<T, Large>(xq, xs, M, K, wq, ws, N, bias, y, st);
+        case Q8Form::t128: return tile_t<T, Middle>(xq, xs, M, K, wq, ws, N, bias, y, st);
+        default: return tile_t<T, Small>(xq, xs, M, K, wq, ws, N, bias, y, st);
+    }
 }
 
 bool product_ok(int dt, int64_t M, int64_t K, const void* wq, const void* ws, int64_t N)
@@ -477,7 +455,7 @@ using namespace scd::lm;
 
 extern "C" {
 
-int64_t scd_q8_stride(int64_t K) { return K < 1 || K > SCD_Q8_MAX_K ? 0 : (K + 127) / 128 * 128; }
+int64_t scd_q8_stride(int64_t K) { return K < 1 || K > SCD_Q8_MAX_K ? 0 : q8_stride(K); }
 
 int scd_q8_rows(const void* X, scd_real dt, int64_t M, int64_t K, int8_t* q, float* s, void* stream)
 {
@@ -499,7 +477,7 @@ int scd_q8_matmul(const int8_t* xq, const float* xs, int64_t M, int64_t K, const
 size_t scd_q8_linear_workspace_bytes(int64_t M, int64_t K)
 {
     if (!rows_ok(M) || K < 1 || K > SCD_Q8_MAX_K) return 0;
-    return M <= 2 && few_owns(M, K) ? 0 : up((size_t)M * (size_t)scd_q8_stride(K), 256) + up((size_t)M * 4, 256);
+    return M <= 2 && q8_few_owns(M, K) ? 0 : up((size_t)M * (size_t)scd_q8_stride(K), 256) + up((size_t)M * 4, 256);
 }
 
 int scd_q8_linear(const void* X, scd_real dt, int64_t M, int64_t K, const int8_t* wq, const float* ws, int64_t N, const void* bias, void* y,
@@ -513,7 +491,7 @@ int scd_q8_linear(const void* X, scd_real dt, int64_t M, int64_t K, const int8_t
     float* xs = (float*)((char*)workspace + up((size_t)M * (size_t)scd_q8_stride(K), 256));
     hipStream_t st = (hipStream_t)stream;
     hipError_t e = hipSuccess;
-    if (const int own = few_takes(M, K, N) ? few_owns(M, K) : 0) {
+    if (const int own = q8_few_takes(M, K, N) ? q8_few_owns(M, K) : 0) {
         e = with_real(dt, [&](auto z) {
             typedef decltype(z) T;
             const FewTokens<T> x{nullptr, nullptr, (const T*)X, aligned16(X) && K * sizeof(T) % 16 == 0};

@@ -1213,123 +1213,8 @@ __global__ __launch_bounds__(QX::kThreads, 2) void xent_grads_tile(DxArgs<T> x, 
 
 // ------------------------------------------------------------------------------------------------ host
 
-constexpr size_t kPieceBytes = (size_t)128 << 20;  // dz of a piece in 16 bits, at most (or of 256 rows)
-constexpr int64_t kTwiceTokens = 64;               // 16-bit types: up to so many tokens, which are bound by memory, dz has twice the
-                                                   // type's digits, so that a gradient is not off by two roundings of one number
-constexpr size_t kCopyBytes = (size_t)1 << 30;     // the copy of a piece of W, at most (or of 256 rows)
-// dW of few tokens from so many bytes on pays for a launch of its own: alone, and beside dX, whose launch it would else share (bf16,
-// 30 tokens, 20000 x 1024: 33 -> 26 us alone, 48 -> 48 with dX; 2 tokens, 32000 x 4096: 171 -> 103, 217 -> 152).
-// (f32: one limit for both, since the f32 instruction gives other bits than the tile's.)
-constexpr int64_t kFewBytes = (int64_t)16 << 20, kFewBesideBytes = (int64_t)128 << 20;
-constexpr int64_t kFewGroups = 768;   // its workgroups, three a compute unit (512 and 1536: the same)
-constexpr int64_t kLeastShare = 8;    // steps
+constexpr int64_t kFewGroups = 768;   // workgroups of xent_dw_few, three a compute unit (512 and 1536: the same)
 constexpr int64_t kWaveLogits = 512;  // logits in shares: up to so many of a token are joined by one wave
-
-// How the tile takes a call of these sizes; the same for the forward and for the gradients.
-struct Shape {
-    int64_t N, D, V;
-    bool f32, split;    // split: f32 on the bf16 instruction
-    int64_t ld;         // entries of a row of the copies
-    int bytes;          // of an entry
-    int dz_planes, dz_bytes;
-
-    bool copies_w;      // W is copied a piece at a time (X always is for the gradients)
-    int64_t piece;      // vocabulary rows of a piece
-    int grads;          // the gradients' tile: 256, 128 or 64, or 0 for the tiles of few tokens
-    int splits;         // shares of the vocabulary that dX is summed in
-    int w_splits;       // shares of the tokens that dW is summed in
-    int z_splits;       // shares of the dims that the logits are summed in
-};
-
-// Whether products of `rows` rows with so many tokens take all tokens in one tile, of 128 rows.
-bool takes_few(int64_t N, int64_t rows) { return N <= 64 && rows > 2048; }
-
-int64_t whole_rows(size_t bytes, size_t bytes_a_row, int64_t V)
-{
-    int64_t rows = (int64_t)(bytes / bytes_a_row) / 256 * 256;
-    if (rows < 256) rows = 256;
-    return rows < V ? rows : V;
-}
-
-// The gradients' tile and the shares that dX is summed in along the vocabulary and dW along the tokens.
-//
-// Few tokens: as many shares of dX as give every compute unit two tiles, of 8 steps at least.  Else both products are one launch, tiles
-// of dX first: it ends, in us, with these or with the work of all on all compute units and half a tile of dW, a step taking about what is
-// measured of it.  Shares are three quarters of that work at most, and cost a launch and their sums' way
-// through memory.  (4000 tokens, 4096 x 200, where dW is few tiles and long: f32 490 us without shares, 115 with them.)
-void choose_grads(Shape& s, int64_t room)
-{
-    const int64_t N = s.N, D = s.D, K = s.piece, row = s.f32 ? 32 : 64;  // entries along k of a step
-    s.splits = s.w_splits = 1;
-    s.grads = 64;
-    if (N <= 0) return;
-    const int64_t x_room = room / (N * s.ld), w_room = K == s.V ? room / (K * s.ld) : 1;
-    auto within = [](int64_t k, int64_t most, int64_t also) {
-        k = k < most ? k : most;
-        k = k < also ? k : also;
-        return k < 1 ? 1 : k;
-    };
-    if (takes_few(N, D)) {
-        s.grads = 0;
-        s.splits = (int)within(512 / cdiv(D, 128), cdiv(K, 64 * kLeastShare), x_room);
-        return;
-    }
-    const int64_t kx = cdiv(K, row), kw = cdiv(N, row);
-    double best = 0;
-    for (int t = row == 32 || s.dz_planes == 2 ? 128 : 256; t >= 64; t /= 2) {
-        const double step = s.split ? (t == 128 ? 0.9 : 0.35) : s.f32 ? (t == 128 ? 1.75 : 0.48) : (t == 256 ? 1.6 : t == 128 ? 0.5 : 0.24) * s.dz_planes;
-        const int64_t nx = cdiv(D, t) * cdiv(N, t), nw = cdiv(D, t) * cdiv(K, t), each = cdiv(nx * kx + nw * kw, 256);
-        const int64_t aim = each * 3 / 4 > kLeastShare ? each * 3 / 4 : kLeastShare;
-        const int64_t sx = within(cdiv(kx, aim), kx / kLeastShare, x_room), sw = within(cdiv(kw, aim), kw / kLeastShare, w_room);
-        for (int shared = 0; shared < 2; ++shared) {
-            if (shared && sx == 1 && sw == 1) break;
-            const int64_t x = shared ? cdiv(kx, sx) : kx, w = shared ? cdiv(kw, sw) : kw, both = each + w / 2;
-            const int64_t sums = shared ? (sx > 1 ? sx * N : 0) + (sw > 1 ? sw * K : 0) : 0;
-            const double cost = (double)(x > both ? x : both) * step + (shared ? 4.0 + 2e-6 * (double)(sums * s.ld) : 0.0);
-            if (best == 0 || cost < best) best = cost, s.grads = t, s.splits = shared ? (int)sx : 1, s.w_splits = shared ? (int)sw : 1;
-        }
-    }
-}
-
-// Shares of the dims for the logits: where a tile a compute unit leaves units without one, and long sums in the others, these take as
-// many shares as end first, in us: whole turns of a tile of 64 (a step takes 0.28 in 16 bits, 0.58 in f32), and with
-// shares one more launch and their sums' way through memory.  (40 tokens, 4096 x 200 in f32: gradients 172 us in one, 52 in 16.)
-int logits_shares_of(const Shape& s, int64_t room)
-{
-    const int64_t ldz = (int64_t)up((size_t)s.V, 64), tiles = takes_few(s.N, s.V) ? cdiv(s.V, 128) : cdiv(s.V, 64) * cdiv(s.N, 64);
-    if (tiles >= 512) return 1;
-    const int64_t steps = cdiv(s.ld * s.bytes, kTileStep);
-    const double step = s.f32 ? 0.58 : 0.28, sums = 8e-6 * (double)(s.N * ldz) / 4;
-    int best = 1;
-    double least = 0;
-    for (int k = 1; k <= 16 && (k == 1 || (k * kLeastShare <= steps && k <= room / (s.N * ldz))); ++k) {
-        const double cost = (double)cdiv(tiles * k, 256) * (double)cdiv(steps, k) * step + (k > 1 ? 5.0 + k * sums : 0.0);
-        if (k == 1 || cost < least) best = k, least = cost;
-    }
-    return best;
-}
-
-Shape shape_of(int dt, int64_t N, int64_t D, int64_t V)
-{
-    Shape s;
-    s.N = N, s.D = D, s.V = V;
-    s.f32 = dt == SCD_REAL_F32;
-    s.split = s.f32 && D >= 64 && V >= 64;  // (sums of a few terms keep all of f32 without)
-    s.ld = (int64_t)up((size_t)D, 8);
-    s.bytes = s.f32 ? 4 : 2;
-    s.copies_w = s.ld != D;
-    s.dz_planes = !s.f32 && N <= kTwiceTokens ? 2 : 1;
-    s.dz_bytes = s.dz_planes == 2 ? 4 : s.bytes;
-    s.piece = whole_rows(kPieceBytes * (s.dz_bytes / 2), (size_t)(N > 0 ? N : 1) * s.dz_bytes, V);
-    if (s.copies_w) {
-        const int64_t w = whole_rows(kCopyBytes, (size_t)s.ld * s.bytes, V);
-        s.piece = w < s.piece ? w : s.piece;
-    }
-    const int64_t room = (int64_t)(kPieceBytes / 4);  // of the sums of shares: no more than a piece
-    choose_grads(s, room);
-    s.z_splits = N > 0 && s.piece == V ? logits_shares_of(s, room) : 1;
-    return s;
-}
 
 // Whether the tile takes operands at these addresses (one that is copied in any case: nullptr).
 bool tile_takes(const Shape& s, const void* X, const void* W)
@@ -1383,15 +1268,14 @@ GradSpace grad_space(const Shape& s)
     return g;
 }
 
-// The tiles.  256 x 256 keeps the matrix cores fed best, and needs a few hundred of them; smaller ones where there are fewer;
-// few tokens take all of them in one tile, deep in flight, and are bound by reading the other operand.
+// The tiles.
 template <class H, bool A, bool B>  // (H: of the operand in more planes)
 using Tile256 = Tile<typename H::Op, 8, 4, 2, 4, A, B, 2, H::P>;
 template <class H, bool A, bool B>
 using Tile128 = Tile<typename H::Op, 4, 4, 2, 2, A, B, 2, H::P>;
 template <class H, bool A, bool B>
 using Tile64 = Tile<typename H::Op, 2, 2, 2, 2, A, B, 3, H::P>;
-// (where a compute unit has one tile at most: its LDS all for that one, steps further ahead; logits of 128 tokens 67 -> 54 us)
+// (one tile a compute unit)
 template <class H, bool A, bool B>
 using Deep128 = Tile<typename H::Op, 4, 4, 2, 2, A, B, 4, H::P>;
 // (of the logits, which take the compute unit for themselves; of dX, which shares it with dW, fewer buffers)
@@ -1408,16 +1292,18 @@ hipError_t few_tile(int64_t tokens, F&& f)
 
 // f(Tile) for the logits of na vocabulary rows and nb tokens.
 template <class H, typename F>
-hipError_t with_tile(int64_t na, int64_t nb, F&& f)
+hipError_t with_tile(const Shape& s, int64_t na, int64_t nb, F&& f)
 {
-    constexpr bool raw32 = std::is_same<H, HeldF32>::value;  // the f32 instruction is slow enough to be fed from any tile
-    constexpr bool wide = sizeof(typename H::In) == 2;  // (values taken apart and their parts leave no registers for a tile of 256)
-    if (takes_few(nb, na)) return few_tile<H, true, true>(nb, f);
-    const int t = raw32 ? pick_tile(na, nb, 1.0, 0.9, 128) : pick_tile(na, nb, 0.8, wide ? 0.45 : 0.5, wide ? 256 : 128);
-    if constexpr (wide)
-        if (t == 256) return f(Tile256<H, true, true>{});
-    if (t == 128 && cdiv(na, t) * cdiv(nb, t) <= 256) return f(Deep128<H, true, true>{});
-    return t == 128 ? f(Tile128<H, true, true>{}) : f(Tile64<H, true, true>{});
+    switch (logits_tile(s, na, nb)) {
+        case LogitsTile::tokens32: return f(Tokens32<H, true, true>{});
+        case LogitsTile::tokens64: return f(Tokens64<H, true, true>{});
+        case LogitsTile::t256:
+            if constexpr (sizeof(typename H::In) == 2) return f(Tile256<H, true, true>{});
+            return hipErrorInvalidConfiguration;  // (16-bit types only)
+        case LogitsTile::deep128: return f(Deep128<H, true, true>{});
+        case LogitsTile::t128: return f(Tile128<H, true, true>{});
+        default: return f(Tile64<H, true, true>{});
+    }
 }
 
 // f(tile of dX, tile of dW): how the gradients are taken.
@@ -1497,7 +1383,7 @@ hipError_t forward_t(const void* X, const void* W, const Shape& s, const void* t
                                        targets, index_bytes, ignore, scale, loss, lse);
                 return hipGetLastError();
             }
-            e = with_tile<H>(piece, N, [&](auto q) {  // (the same tile for every piece: the strips are its)
+            e = with_tile<H>(s, piece, N, [&](auto q) {  // (the same tile for every piece: the strips are its)
                 typedef decltype(q) Q;
                 static_assert(16 * Q::FA >= kLeastStrip && 256 % (16 * Q::FA) == 0, "the work space holds so many strips, pieces whole ones");
                 nstrips = cdiv(V, 16 * Q::FA);
@@ -1588,7 +1474,7 @@ hipError_t grad_tile_t(const GradArgs& a, const Shape& s, const GradSpace& sp, h
                                    rows, active, dz, ldz);
                 e = hipGetLastError();
             } else {
-                e = with_tile<H>(width, N, [&](auto q) {
+                e = with_tile<H>(s, width, N, [&](auto q) {
                     typedef decltype(q) Q;
                     return launch_tiles<Q>(xent_dz_tile<T, HZ, Q>, width, N, 1, st, w, x, v0, a.scale, rows, active, dz, ldz);
                 });
@@ -1603,7 +1489,8 @@ hipError_t grad_tile_t(const GradArgs& a, const Shape& s, const GradSpace& sp, h
         bool rest = a.dW;  // dW is still to be made
         {
             typedef DwFew<T, HZ, HZ::P == 2 ? 1 : 2> F;
-            if (rest && N > 0 && N <= F::kTokens && width * D * (int64_t)sizeof(T) >= (a.dX || sizeof(T) == 4 ? kFewBesideBytes : kFewBytes)) {
+            static_assert(F::kTokens == (sizeof(T) == 4 || HZ::P == 2 ? 64 : 128), "as many tokens as walk_tokens says");
+            if (rest && dw_walks(s, width, a.dX)) {
                 const int64_t nd = cdiv(D, F::SideX::T), stretches = cdiv(width, F::SideZ::T), groups = cdiv(kFewGroups, nd);
                 const int64_t grid = nd * (groups < stretches ? groups : stretches);
                 if (!grid_ok(grid, F::kThreads)) return hipErrorInvalidConfiguration;
