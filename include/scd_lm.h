@@ -70,7 +70,7 @@ int scd_q8_linear(const void* X, scd_real dt, int64_t M, int64_t K, const int8_t
  * loss is 0 where t_i == ignore, NaN where t_i is another value outside 0 .. V-1.  A logit that is NaN or +infinity makes its
  * row's lse and loss NaN.  In f32, D and V from 64 on, products are of three parts of bf16: entries below 2^-102 may lose some
  * of their 24 bits, finite ones beyond 3.39e38 may be taken for that.  Logits are formed tile by
- * tile and not kept: the work space holds a few sums for each row and tile (and, where there are few logits in all, these). */
+ * tile and not kept: the work space holds two sums for each row and up to 128 of the vocabulary (where there are few logits in all: these). */
 size_t scd_xent_workspace_bytes(scd_real dt, int64_t N, int64_t D, int64_t V);
 int scd_xent(const void* X, const void* W, scd_real dt, int64_t N, int64_t D, int64_t V, const void* targets, int index_bytes,
              int64_t ignore, float scale, float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -140,8 +140,7 @@ __device__ __forceinline__ void tile32(const Operand<TA>& A, const Operand<TB>& 
 
 // ------------------------------------------------------------------------------------------------ forward
 
-constexpr int kStrip = 64;   // vocabulary rows behind one pair of sums of a token, in tile32
-constexpr int kLeastStrip = 32;  // and at least
+constexpr int kStrip = kT;  // vocabulary rows behind one pair of sums of a token, in tile32
 
 struct Sums {
     float max, sum;  // of the logits, and of exp(logit - max)
@@ -153,11 +152,13 @@ __global__ __launch_bounds__(kTThreads) void xent_forward32(Operand<T> W, Operan
                                                             Sums* __restrict__ strips, float* __restrict__ zt)
 {
     __shared__ TileLds sh;
+    __shared__ Sums lower[kT];  // of the tile's lower half
     const int64_t v0 = (int64_t)blockIdx.x * kT, n0 = (int64_t)blockIdx.y * kT;
     v4f acc[4][4];
     tile32<true, true>(W, X, v0, n0, W.inner, sh, acc);
     const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
     const int li = lane & 15, kq = lane >> 4, wr = (wv >> 1) * 64, wc = (wv & 1) * 64;
+    Sums half[4];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
         const int64_t n = n0 + wc + b * 16 + li;
@@ -185,12 +186,22 @@ __global__ __launch_bounds__(kTThreads) void xent_forward32(Operand<T> W, Operan
             }
         sum += __shfl_xor(sum, 16, kWave);
         sum += __shfl_xor(sum, 32, kWave);
-        if (kq == 0 && live && v0 + wr < W.outer) {
-            Sums s;
-            s.max = top;
-            s.sum = sum;
-            strips[(v0 + wr) / kStrip * X.outer + n] = s;
-        }
+        half[b].max = top;
+        half[b].sum = sum;
+        if (wr && kq == 0) lower[wc + b * 16 + li] = half[b];
+    }
+    __syncthreads();
+    if (wr || kq) return;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const int64_t n = n0 + wc + b * 16 + li;
+        if (n >= X.outer) continue;
+        const Sums x = half[b], y = lower[wc + b * 16 + li];
+        Sums s;
+        s.max = fmaxf(x.max, y.max);
+        const float base = s.max == -__builtin_inff() ? 0.0f : s.max;
+        s.sum = x.sum * expf(x.max - base) + y.sum * expf(y.max - base);
+        strips[v0 / kStrip * X.outer + n] = s;
     }
 }
 
@@ -1216,12 +1227,9 @@ __global__ __launch_bounds__(QX::kThreads, 2) void xent_grads_tile(DxArgs<T> x, 
 constexpr int64_t kFewGroups = 768;   // workgroups of xent_dw_few, three a compute unit (512 and 1536: the same)
 constexpr int64_t kWaveLogits = 512;  // logits in shares: up to so many of a token are joined by one wave
 
-// Whether the tile takes operands at these addresses (one that is copied in any case: nullptr).
-bool tile_takes(const Shape& s, const void* X, const void* W)
-{
-    if (s.ld * s.bytes > kTileMaxPitch) return false;
-    return s.copies_w || (aligned16(X) && aligned16(W));
-}
+// Whether the tile takes rows of this length, and operands at these addresses (one that is copied in any case: nullptr).
+bool tile_reaches(const Shape& s) { return s.ld * s.bytes <= kTileMaxPitch; }
+bool tile_takes(const Shape& s, const void* X, const void* W) { return tile_reaches(s) && (s.copies_w || (aligned16(X) && aligned16(W))); }
 
 struct ForwardSpace {
     size_t zt, strips, z, x, w, bytes;
@@ -1229,14 +1237,20 @@ struct ForwardSpace {
 
 size_t logits_bytes(const Shape& s) { return s.z_splits > 1 ? up(s.z_splits * (size_t)s.N * up((size_t)s.V, 64) * 4, 256) : 0; }
 
+// Vocabulary rows that the forward takes at once.
+int64_t forward_piece(const Shape& s) { return s.copies_w ? s.piece : s.V; }
 
+// One layout for whichever form runs, since addresses have a say in that: strips of the tile or of tile32, or shares of the logits.
 ForwardSpace forward_space(const Shape& s)
 {
     ForwardSpace f;
+    auto strips = [&](int64_t rows) { return up((size_t)cdiv(s.V, rows) * (size_t)s.N * sizeof(Sums), 256); };
+    size_t most = 0;
+    if (tile_reaches(s)) most = s.z_splits > 1 ? logits_bytes(s) : strips(strip_rows(logits_tile(s, forward_piece(s), s.N)));
+    if (!s.copies_w || !tile_reaches(s)) most = strips(kStrip) > most ? strips(kStrip) : most;
     f.zt = 0;
-    f.strips = up((size_t)s.N * 4, 256);
-    f.z = f.strips + up((size_t)cdiv(s.V, kLeastStrip) * (size_t)s.N * sizeof(Sums), 256);
-    f.x = f.z + logits_bytes(s);
+    f.strips = f.z = up((size_t)s.N * 4, 256);
+    f.x = f.z + most;
     f.w = f.x + (s.copies_w ? up((size_t)s.N * (size_t)s.ld * s.bytes, 256) : 0);
     f.bytes = f.w + (s.copies_w ? up((size_t)s.piece * (size_t)s.ld * s.bytes, 256) : 0) + 256;
     return f;
@@ -1365,7 +1379,7 @@ hipError_t forward_t(const void* X, const void* W, const Shape& s, const void* t
     if (tile_takes(s, X, W)) {
         if (s.copies_w && (e = lay_out_rows<T, H>((const T*)X, N, D, ws + sp.x, s.ld, st)) != hipSuccess) return e;
         const TileRows x = rows_of<H>(s.copies_w ? ws + sp.x : X, N, s.ld);
-        const int64_t piece = s.copies_w ? s.piece : V;
+        const int64_t piece = forward_piece(s);
         for (int64_t v0 = 0; v0 < V; v0 += piece) {
             const int64_t width = V - v0 < piece ? V - v0 : piece;
             const T* from = (const T*)W + v0 * D;
@@ -1385,7 +1399,8 @@ hipError_t forward_t(const void* X, const void* W, const Shape& s, const void* t
             }
             e = with_tile<H>(s, piece, N, [&](auto q) {  // (the same tile for every piece: the strips are its)
                 typedef decltype(q) Q;
-                static_assert(16 * Q::FA >= kLeastStrip && 256 % (16 * Q::FA) == 0, "the work space holds so many strips, pieces whole ones");
+                static_assert(256 % (16 * Q::FA) == 0, "pieces hold whole strips");
+                if (strip_rows(logits_tile(s, piece, N)) != 16 * Q::FA) return hipErrorInvalidConfiguration;  // (the work space holds so many)
                 nstrips = cdiv(V, 16 * Q::FA);
                 return launch_tiles<Q>(xent_forward_tile<Q>, width, N, 1, st, w, x, v0, targets, index_bytes, scale, strips, zt);
             });

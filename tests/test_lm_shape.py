@@ -53,3 +53,15 @@ def test_the_gpu_tests_reach_every_form_of_the_8_bit_products(forms):
     all_of = needed(forms([("q8", *s) for s in sizes]))
     tested = forms([("q8", *s) for s in Q8])
     assert len(all_of) >= 9 and all_of <= tested, sorted(all_of - tested)
+
+
+@pytest.mark.parametrize("dtype", [0, 2, 3])
+@pytest.mark.parametrize("N,D,V", [(4096, 4096, 32000), (16384, 4096, 128256), (32768, 1024, 128256), (1, 4096, 32000), (2048, 2048, 200)])
+def test_work_space_of_the_loss_is_two_sums_for_each_row_and_strip(dtype, N, D, V):
+    """8 bytes for each token and 128 rows of the vocabulary (tiles of 128, as f32 takes them: 64; of few tokens: 32), besides what is rounded up.
+    Logits in shares: up to 16 of them."""
+    from paper_2410_01799_amd import scd
+
+    strip = 32 if N <= 64 else 64 if dtype == 0 else 128
+    most = -(-V // strip) * N * 8 if V > 2048 else 16 * N * 4 * (V + 64)
+    assert scd.lib().scd_xent_workspace_bytes(dtype, N, D, V) <= most + 4 * N + 4096
