@@ -392,7 +392,9 @@ def scd_release_memory() -> int:
 # --------------------------------------------------------------------------- around the matrices of a language model
 #
 # These calls enqueue their work on the current stream and return (include/scd_lm.h).  Work space comes from torch's allocator
-# unless it is given; it may be used again by later calls on the same stream.
+# unless it is given; it may be used again by later calls on the same stream.  torch's autograd does not see them: gradients are calls
+# of their own (scd_embed_grad, scd_xent_grad), and an array that asks for one is refused rather than left without it (but by
+# scd_q8_rows, which makes integers).
 
 
 def _real(t: torch.Tensor, name: str, dtype: Optional[torch.dtype] = None) -> int:
@@ -441,6 +443,12 @@ def _space(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor):
 _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (the call behind current_device, without its checks)
 
 
+def _no_autograd(name: str, *arrays: Optional[torch.Tensor]):
+    for t in arrays:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} is not recorded by autograd: call it under torch.no_grad() or with detached arrays")
+
+
 def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]):
     d = first.get_device()
     for t in others:
@@ -452,6 +460,7 @@ def _same_device(first: torch.Tensor, *others: Optional[torch.Tensor]):
 
 def scd_embed(E: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0) -> torch.Tensor:
     """scale * E[tokens]: rows of E (V x D) for tokens of any shape (int32 or int64); NaN rows for tokens outside 0 .. V-1."""
+    _no_autograd("scd_embed", E)
     dt, ib = _real(_matrix(E, "E"), "E"), _index(tokens, "tokens")
     _same_device(E, tokens)
     V, D = E.shape
@@ -468,6 +477,7 @@ def scd_embed_grad(tokens: torch.Tensor, dY: torch.Tensor, V: int, scale: float 
                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of scd_embed in E (V x D, dtype of dY) from that in its result, dY (shape of tokens, D).  Tokens equal to
     pad or outside 0 .. V-1 count for nothing."""
+    _no_autograd("scd_embed_grad", dY)
     dt, ib = _real(_dev(dY, "dY"), "dY"), _index(tokens, "tokens")
     if dY.dim() < 1 or dY.shape[:-1] != tokens.shape:
         raise ValueError("dY must have the shape of tokens and one dimension more")
@@ -510,6 +520,7 @@ def scd_q8_linear(X: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, bias: Opt
                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """X (..., K) times the transpose of N x K weights held in 8 bits (scd_q8_rows of them), plus bias: (..., N), dtype of X.
     The rows of X are put into 8 bits on the way."""
+    _no_autograd("scd_q8_linear", X, ws, bias)
     dt = _real(_dev(X, "X"), "X")
     if X.dim() < 1:
         raise ValueError("X must have a last dimension")
@@ -527,6 +538,7 @@ def scd_q8_linear(X: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, bias: Opt
 def scd_q8_matmul(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, K: int, dtype: torch.dtype = torch.bfloat16,
                   bias: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The same from tokens already in 8 bits (xq, xs = scd_q8_rows(X)), as several projections of one X share them."""
+    _no_autograd("scd_q8_matmul", xs, ws, bias)
     if dtype not in REALS:
         raise TypeError(f"dtype {dtype} not supported (float32, bfloat16 or float16)")
     _matrix(xq, "xq")
@@ -560,6 +572,7 @@ def scd_xent(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, ignore: in
              workspace: Optional[torch.Tensor] = None):
     """(loss, lse), float32, one for each row of X: lse = log sum exp of the logits scale * X W^T, loss = lse minus the target's
     logit (0 where the target is ignore)."""
+    _no_autograd("scd_xent", X, W)
     dt, ib, N, D, V = _xent_shapes(X, W, targets)
     _same_device(X, W, targets, workspace)
     ws, ws_bytes, _held = _space(workspace, lib().scd_xent_workspace_bytes(dt, N, D, V), X)
@@ -576,6 +589,7 @@ def scd_xent_grad_workspace_bytes(dtype: torch.dtype, N: int, D: int, V: int) ->
 def scd_xent_grad(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, g: torch.Tensor, ignore: int = -100,
                   scale: float = 1.0, want_dX: bool = True, want_dW: bool = True, workspace: Optional[torch.Tensor] = None):
     """(dX, dW): gradients of sum_i g_i loss_i in X and W (None for one that is not wanted); lse is scd_xent's."""
+    _no_autograd("scd_xent_grad", X, W, lse, g)
     dt, ib, N, D, V = _xent_shapes(X, W, targets)
     _typed(lse, "lse", torch.float32, (N,))
     _typed(g, "g", torch.float32, (N,))
