@@ -50,13 +50,23 @@ inline int q8_few_owns(int64_t M, int64_t K)
     return M <= kQ8FewTokens && M * row <= kQ8ManyLds ? kQ8FewTokens : 0;
 }
 
-// Whether q8_few_kernel takes so many tokens at all.  It reads a few MiB at once with the least latency; large weights stream
-// faster through the tile once there is more than a token or two to multiply them with (measured: 14336 x 14336, 4 tokens, 54 us
-// here and 40 there; 14336 x 4096, 16 tokens, 25 and 22, 8 tokens 21 and 22; 4096 x 14336, 16 tokens, 27 and 32).
+// Whether q8_few_kernel takes so many tokens at all.  It has the least latency and reads long rows by many waves each; its channels come in
+// turns of 8192, which cost 4 us each however short the rows, and from three tokens on putting them into 8 bits is on its way, too.  The
+// tile takes 5 us and the larger of 2.1 us for 1000 entries of a row and reading the weights at 5.6 TB/s.  Measured, us, here / tile, weights from
+// memory (bf16; K -> N at 3, 8 and 16 tokens):
+//     1024 ->  4096    7.9 /  7.7    7.2 /  7.9    9.2 /  8.0       8192 ->  4096   14.0 / 22.3   17.4 / 22.4   16.0 / 22.7
+//     1024 ->  6144   11.1 /  8.5   10.4 /  8.7   13.1 /  8.8       8192 ->  8192   19.4 / 23.2   23.0 / 23.5   24.6 / 23.8
+//     4096 ->  1024    8.3 / 12.3    8.3 / 12.6   11.4 / 12.6       8192 -> 14336   27.5 / 26.8   32.9 / 26.9   40.0 / 27.2
+//     4096 ->  4096   10.1 / 14.1   10.0 / 14.4   13.4 / 14.5      14336 ->  4096   26.5 / 34.6   22.1 / 34.9   24.9 / 35.3
+//     4096 ->  7168   13.7 / 14.6   14.4 / 14.8   16.7 / 15.1      14336 ->  6144   33.8 / 36.0   33.7 / 36.2   39.1 / 36.9
+//     4096 ->  8192   14.2 / 14.8   15.1 / 14.9   17.2 / 15.3      14336 ->  8192   36.4 / 37.5   35.3 / 37.8   40.6 / 38.5
+//     4096 -> 14336   17.5 / 16.8   18.9 / 16.8   23.7 / 17.0      14336 -> 14336   54.5 / 43.8   60.1 / 44.1   71.3 / 44.5
+//     2048 ->  8192   11.4 / 10.6   11.5 / 10.8   15.0 / 10.9      32768 ->  4096   62.2 / 69.6   50.5 / 69.8   53.4 / 70.8
+// One or two tokens stay here always, since they need no work space (mostly faster too: 4096 -> 4096 7.6 / 14.0, 14336 -> 14336 42.6 / 43.7; slower
+// where short rows are many: 2048 -> 64000 40 / 28).
 inline bool q8_few_takes(int64_t M, int64_t K, int64_t N)
 {
-    const int64_t bytes = N * q8_stride(K);
-    return M <= kQ8FewTokens && !(M > 2 && bytes >= (96 << 20)) && !(M > 8 && N >= 8192 && bytes >= (48 << 20));
+    return M <= 2 || (M <= kQ8FewTokens && N < 8192 && (N <= 4096 || K > 2048));
 }
 
 enum class Q8Form { few, narrow, t256, t128, t64 };  // narrow: tiles of 64 channels and 32 tokens
