@@ -18,7 +18,9 @@
  *    f32 throughout).
  *  - Row counts may be 0 (nothing to do; gradients of weights are then zero).
  *  - SCD_EINVAL: null pointers, sizes below 1 (row counts: below 0) or above 2^31 - 1, an unknown type, a work space that
- *    is too small or misaligned.  SCD_EHIP: a launch failed.  Nothing is enqueued on SCD_EINVAL.
+ *    is too small or misaligned.  SCD_EHIP: a launch failed (a call that takes 2^32 threads or more does: rows of odd lengths
+ *    from about 2^34 entries on, cross entropy from 2^26 tokens or rows of the vocabulary on, embedding gradients from 2^28 rows on).
+ *    Nothing is enqueued on SCD_EINVAL.
  */
 #ifndef SCD_LM_H
 #define SCD_LM_H
@@ -58,8 +60,8 @@ int scd_q8_rows(const void* X, scd_real dt, int64_t M, int64_t K, int8_t* q, flo
 int scd_q8_matmul(const int8_t* xq, const float* xs, int64_t M, int64_t K, const int8_t* wq, const float* ws, int64_t N,
                   const void* bias, scd_real dt, void* y, void* stream);
 
-/* The same from tokens that are not yet in 8 bits: scd_q8_rows of X (M x K, dt), then scd_q8_matmul; same bits.  One or two
- * tokens need no work space (0 bytes; it may then be NULL). */
+/* The same from tokens that are not yet in 8 bits: scd_q8_rows of X (M x K, dt), then scd_q8_matmul; same bits.  One
+ * token of up to about 114,000 entries and two of up to 57,000 need no work space (0 bytes; it may then be NULL). */
 size_t scd_q8_linear_workspace_bytes(int64_t M, int64_t K);
 int scd_q8_linear(const void* X, scd_real dt, int64_t M, int64_t K, const int8_t* wq, const float* ws, int64_t N, const void* bias,
                   void* y, void* workspace, size_t workspace_bytes, void* stream);
