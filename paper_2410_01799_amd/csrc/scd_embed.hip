@@ -429,8 +429,10 @@ hipError_t embed_grad_t(const void* tokens, int index_bytes, int64_t N, const vo
     hipLaunchKernelGGL(embed_sort, dim3((unsigned)cdiv(V, kSortRows)), dim3(kSortThreads), 0, st, tokens, index_bytes, N, V, pad, so);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // Rows of dE written past the caches leave these to dY, which frequent tokens' rows and their neighbours are read from (16384 tokens,
-    // 32000 x 4096 bf16: 130 -> 89 us); with few tokens to a row writing is all there is to do (300: 48 us through them, 61 past).
+    // Rows of dE written past the caches leave these to dY, which frequent tokens' rows and their neighbours are read from (32000 x 4096
+    // bf16, a call of 16384 tokens 127 -> 113 us, of 4096 90 -> 69, of 1000 79 -> 65).  With fewer tokens to a row writing is all there is to
+    // do, and a dE that is written again and again is still in the last cache (300 tokens: 48 us through the caches, 61 past; of three dE in turn
+    // 66 and 58).
     auto kernel = N >= V / 32 ? embed_rows<T, VN, true> : embed_rows<T, VN, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)((row_groups + piece_groups) * sh.slices)), dim3(kRowThreads), 0, st, (const T*)dY, V, D, so.start, so.order,
                        so.first, sh, piece_groups, scale, (T*)dE, parts);

@@ -1090,7 +1090,7 @@ __device__ __forceinline__ void dw_tile(char* lds, int64_t block, const DwArgs<T
 // in registers and walks along the vocabulary, 64 rows at a time: dz of the rows two stretches ahead is on its way to LDS while the
 // products of these are rounded there and written out, 256 or 512 bytes of a row at once, past the caches: they hold no gradient of
 // this size for its reader, but much of W for the next product.  (32000 x 4096 bf16, two tokens: 93 us by dw_tile, whose workgroups
-// each wait for their own operands, 45 here; a fill takes 38.)
+// each wait for their own operands, 53 here; a fill takes 38.)
 template <typename T, class H, int STEPS>
 struct DwFew {
     // (f32 as it is: with few tokens the f32 instruction keeps up)
